@@ -425,9 +425,10 @@ struct Side {
 
 // Instructions come next after HBM (120 a token took 94 us at 4096 x 4096, 67 took 48, 40 take
 // 39): what is the same for all tokens is asked once a unit, a warp whose tokens all count
-// tests none of them, two values go through one instruction where they can, and a token that
-// does not count is one with log ratios 0: its ratio is 1, inside every clipping range, so
-// that a count corrects the sums it went into.
+// tests none of them, and two values go through one instruction where they can. A token that
+// does not count has log ratios 0: its ratio is 1, inside every clipping range, and is dropped
+// before the sums (adding it and taking a count of them out again would leave an absolute
+// error, which small ratios behind a scattered mask vanish in).
 template <int MODE>
 struct PolicyChunk {
   uint32_t bits;
@@ -478,7 +479,6 @@ struct PolicyChunk {
     for (int k = 0; k < kE; ++k) g[k] = 0.f;
     if (live) {
       const uint32_t n = __popc(bits);
-      const float out = (float)(kE - n);   // tokens that do not count
       t.tok += n;
       if (a.token_adv) {
         float pg = 0.f, rat = 0.f;
@@ -491,10 +491,10 @@ struct PolicyChunk {
           t.low += clipped && sd.s < 0.f ? 1u : 0u;
           t.high += clipped && sd.s > 0.f ? 1u : 0u;
           g[k] = clipped ? 0.f : -(sd.mag * w) * x;
-          rat += r;
+          rat += (bits >> k) & 1u ? r : 0.f;
         }
         t.pg -= w * pg;
-        t.rat += rat - out;
+        t.rat += rat;
       } else {
         const Side sd(a, A_row);
         const float mw = sd.mag * w;
@@ -519,15 +519,17 @@ struct PolicyChunk {
             const bool c0 = x[0] > sd.bound, c1 = x[1] > sd.bound;
             clips += c0 ? 1u : 0u;
             clips += c1 ? 1u : 0u;
-            sr = add2(sr, x2);
+            x[0] = (bits >> k) & 1u ? x[0] : 0.f;
+            x[1] = (bits >> (k + 1)) & 1u ? x[1] : 0.f;
+            sr = add2(sr, Two(x[0], x[1]));
             sp = add2(sp, Two(c0 ? sd.bound : x[0], c1 ? sd.bound : x[1]));
             mul2(Two(-mw, -mw), Two(c0 ? 0.f : x[0], c1 ? 0.f : x[1])).get(g[k], g[k + 1]);
           }
           float odd;
           sp.get(pg, odd);
-          pg += odd - sd.s * out;
+          pg += odd;
           sr.get(rat, odd);
-          rat += odd - sd.s * out;
+          rat += odd;
         }
         // (a lane without tokens adds nothing, whatever its row's values are)
         if (n > 0) {
