@@ -364,4 +364,31 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
+// A running sum and what its roundings have left out (Knuth's two-sum; single roundings, so
+// that no product of the caller's is fused into it).
+struct alignas(8) Sum2 {
+  float s, c;
+  __device__ __forceinline__ void add(float x) {
+    const float t = __fadd_rn(s, x), xs = __fsub_rn(t, s);
+    c += __fsub_rn(s, __fsub_rn(t, xs)) + __fsub_rn(x, xs);
+    s = t;
+  }
+  __device__ __forceinline__ void add(const Sum2& o) {
+    add(o.s);
+    c += o.c;
+  }
+  // Over the lanes of a warp, the same in all of them.
+  __device__ __forceinline__ void over_warp() {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      Sum2 q;
+      q.s = __shfl_xor_sync(0xffffffffu, s, o);
+      q.c = __shfl_xor_sync(0xffffffffu, c, o);
+      add(q);
+    }
+  }
+  // (an infinite or NaN sum has a NaN remainder)
+  __device__ __forceinline__ float value() const { return isfinite(s) ? s + c : s; }
+};
+
 }  // namespace bgpo

@@ -115,30 +115,6 @@ __device__ __forceinline__ int64_t unit_begin(const GradTensor& t, uint32_t u) {
   return (int64_t)(u - t.begin) * kGradUnit - t.shift;
 }
 
-// A running sum and what its roundings have left out (Knuth's two-sum).
-struct Sum2 {
-  float s = 0.f, c = 0.f;
-  __device__ __forceinline__ void add(float x) {
-    const float t = s + x, xs = t - s;
-    c += (s - (t - xs)) + (x - xs);
-    s = t;
-  }
-  __device__ __forceinline__ void add(const Sum2& o) {
-    add(o.s);
-    c += o.c;
-  }
-  // Over the lanes of a warp, the same in all of them.
-  __device__ __forceinline__ void over_warp() {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      Sum2 q;
-      q.s = __shfl_xor_sync(0xffffffffu, s, o);
-      q.c = __shfl_xor_sync(0xffffffffu, c, o);
-      add(q);
-    }
-  }
-};
-
 // Sum of squares of this thread's elements of a unit that starts at element e0.
 template <class T>
 __device__ __forceinline__ float unit_squares(const GradTensor& t, int64_t e0) {
@@ -178,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 4)
     k_grad_norm(const __grid_constant__ GradList<CAP> l, GradNormArgs a) {
   pdl_begin();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  Sum2 mine;
+  Sum2 mine = {};
   for (uint32_t u = blockIdx.x; u < l.units; u += gridDim.x) {
     const GradTensor& t = l.t[tensor_of(l, u)];
     const int64_t e0 = unit_begin(t, u);
@@ -200,13 +176,10 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
   __syncthreads();
   if (!s_last) return;
-  mine = Sum2{};
+  mine = {};
   for (int b = threadIdx.x; b < (int)gridDim.x; b += kThreads) {
     const float2 q = __ldcg(&a.w.squares[1 + b]);
-    Sum2 x;
-    x.s = q.x;
-    x.c = q.y;
-    mine.add(x);
+    mine.add(Sum2{q.x, q.y});
   }
   mine.over_warp();
   if (lane == 0) s_warp[warp] = mine;
@@ -214,15 +187,12 @@ __global__ void __launch_bounds__(kThreads, 4)
   if (threadIdx.x != 0) return;
   for (int i = 1; i < kWarps; ++i) mine.add(s_warp[i]);
   if (!a.first) {                    // the launches before this one, of the same call
-    Sum2 x;
-    x.s = a.w.squares[0].x;
-    x.c = a.w.squares[0].y;
-    mine.add(x);
+    const float2 q = a.w.squares[0];
+    mine.add(Sum2{q.x, q.y});
   }
   a.w.squares[0] = make_float2(mine.s, mine.c);
   if (a.last) {
-    // an infinite or NaN sum has a NaN remainder
-    const float norm = sqrtf(isfinite(mine.s) ? mine.s + mine.c : mine.s);
+    const float norm = sqrtf(mine.value());
     *a.norm = norm;
     if (!isfinite(norm)) set_device_error(a.w.err, kStatusNonfinite, KID_GRAD_NORM * 16);
   }

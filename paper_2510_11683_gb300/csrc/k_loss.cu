@@ -314,12 +314,15 @@ __device__ __forceinline__ bool grid_totals(const TrainWs& w, LossTotals& t) {
   __syncthreads();
   if (!s_last) return false;
   t = LossTotals{};
+  Sum2 sum[4] = {};
   for (int b = threadIdx.x; b < (int)gridDim.x; b += blockDim.x) {
     const float4 f = __ldcg(reinterpret_cast<const float4*>(w.sums[b].f));
-    t.f[0] += f.x; t.f[1] += f.y; t.f[2] += f.z; t.f[3] += f.w;
+    sum[0].add(f.x); sum[1].add(f.y); sum[2].add(f.z); sum[3].add(f.w);
 #pragma unroll
     for (int i = 0; i < 3; ++i) t.c[i] += __ldcg(&w.sums[b].c[i]);
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t.f[i] = sum[i].value();
   block_totals(t, s_t);
   return threadIdx.x == 0;
 }
@@ -408,9 +411,25 @@ __device__ __forceinline__ Two exp_rest2(Two k) {
   return mul2(mul2(k, k), p);
 }
 
+// A thread's sums over all its units. They carry what their roundings leave out: a chain of
+// plain additions grows with the batch (2 x 10^4 equal ones: 1.6e-4 off).
+// Blocks, whose 64 registers a thread are full, keep them in shared memory (32 bytes of spills
+// a thread instead of 112 for rows in vectors).
+enum PolicySum : int { kPg = 0, kKl = 1, kRat = 2 };
+template <bool BLOCK>
 struct PolicySums {
-  float pg = 0.f, kl = 0.f, rat = 0.f;
+  Sum2 q[BLOCK ? 1 : 3];
+  Sum2* slot;    // of this thread: sum i is slot[i * blockDim.x]
   uint32_t low = 0, high = 0, tok = 0;
+  __device__ __forceinline__ explicit PolicySums(Sum2* slots) : slot(slots + threadIdx.x) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) at(i) = {};
+  }
+  __device__ __forceinline__ Sum2& at(int i) {
+    return BLOCK ? slot[i * blockDim.x] : q[BLOCK ? 0 : i];
+  }
+  __device__ __forceinline__ void add(PolicySum i, float x) { at(i).add(x); }
+  __device__ __forceinline__ float value(PolicySum i) { return at(i).value(); }
 };
 
 // An advantage as its magnitude and a sign s: with x = s r, a token's term is -|A| min(x,
@@ -465,15 +484,19 @@ struct PolicyChunk {
       adv[k] = m ? adv[k] : 0.f;
     }
   }
-  __device__ __forceinline__ void add_log_ratios(float& s) const {
-    if (!live) return;
+  __device__ __forceinline__ float log_ratios() const {   // their sum
+    float s = 0.f;
+    if (live) {
 #pragma unroll
-    for (int k = 0; k < kE; ++k) s += d[k];
+      for (int k = 0; k < kE; ++k) s += d[k];
+    }
+    return s;
   }
   // Gradients of the chunk's tokens, and what they add to the sums. w: weight of a token;
   // A_row, r_row: the row's advantage and ratio where they are one a row.
+  template <bool BLOCK>
   __device__ __forceinline__ void finish(const PolicyArgs& a, const Span<MODE>& c, float w,
-                                         float A_row, float r_row, PolicySums& t) {
+                                         float A_row, float r_row, PolicySums<BLOCK>& t) {
     float g[kE];
 #pragma unroll
     for (int k = 0; k < kE; ++k) g[k] = 0.f;
@@ -493,8 +516,8 @@ struct PolicyChunk {
           g[k] = clipped ? 0.f : -(sd.mag * w) * x;
           rat += (bits >> k) & 1u ? r : 0.f;
         }
-        t.pg -= w * pg;
-        t.rat += rat;
+        t.add(kPg, -w * pg);
+        t.add(kRat, rat);
       } else {
         const Side sd(a, A_row);
         const float mw = sd.mag * w;
@@ -533,8 +556,8 @@ struct PolicyChunk {
         }
         // (a lane without tokens adds nothing, whatever its row's values are)
         if (n > 0) {
-          t.pg -= mw * pg;
-          t.rat += sd.s * rat;
+          t.add(kPg, -mw * pg);
+          t.add(kRat, sd.s * rat);
         }
         t.low += sd.s < 0.f ? clips : 0u;
         t.high += sd.s < 0.f ? 0u : clips;
@@ -564,7 +587,7 @@ struct PolicyChunk {
             kr[k] = near ? x + q : e1;
           }
         }
-        t.kl += w * kl;
+        t.add(kKl, w * kl);
         if (a.beta != 0.f) {
           const float bw = -a.beta * w;
 #pragma unroll
@@ -608,9 +631,10 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
   } else if (a.norm == BGPO_NORM_ROWS) {
     w = a.scale / ((float)a.N * (float)a.T);   // without a mask
   }
-  PolicySums t;
-  PolicyChunk<MODE> x;
   constexpr bool BLOCK = TEAM >= kBlock, sums_rows = TEAM != kNone;
+  extern __shared__ Sum2 s_sums[];   // (blocks: 3 a thread)
+  PolicySums<BLOCK> t(s_sums);
+  PolicyChunk<MODE> x;
   __shared__ typename TeamSums<1>::Shared s_team;
   const uint32_t cl = TEAM >= kCluster ? a.cluster : 1;
   const uint32_t rank = TEAM >= kCluster ? cluster_ctarank() : 0;
@@ -656,7 +680,7 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
         float s[1] = {0.f};
         if (a.sequence) {
           x.ratios(a);
-          x.add_log_ratios(s[0]);
+          s[0] = x.log_ratios();
         }
         sums.template sum<TEAM>(n, s, a.sequence);
         const float nf = (float)max(n[0], 1);
@@ -671,16 +695,17 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
     for (; u < units; u += step) {
       const float A_row = a.token_adv ? 0.f : a.adv.p[u * a.adv.row];
       int32_t n[1] = {0};
-      float s[1] = {0.f};
+      Sum2 row = {};
       uint32_t c0 = chunk0;
       do {
         const Span<MODE> c(u, c0, threads, tid, a.T, a.lp.row, a.phase);
         x.load(a, c, load_mask<MODE>(a.mask, c));
         x.ratios(a);
         n[0] += __popc(x.bits);
-        if (a.sequence) x.add_log_ratios(s[0]);
+        if (a.sequence) row.add(x.log_ratios());
         c0 += stride;
       } while (c0 < (uint32_t)a.T + 7);
+      float s[1] = {row.value()};
       sums.template sum<TEAM>(n, s, a.sequence);
       const float nf = (float)max(n[0], 1);
       const float wr = a.norm == BGPO_NORM_ROWS ? a.scale / ((float)a.N * nf) : w;
@@ -699,7 +724,7 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
     __syncwarp();
     cluster_sync();
   }
-  LossTotals all = {{t.pg, t.kl, t.rat, 0.f}, {t.low, t.high, t.tok}};
+  LossTotals all = {{t.value(kPg), t.value(kKl), t.value(kRat), 0.f}, {t.low, t.high, t.tok}};
   if (!grid_totals(a.w, all)) return;
   const float n = (float)max(all.c[2], 1ull);
   const float loss = a.beta != 0.f ? all.f[0] + a.beta * all.f[1] : all.f[0];
@@ -753,7 +778,14 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
   const uint32_t chunk0 = rank * (uint32_t)threads * kE, stride = cl * (uint32_t)threads * kE;
   const float unit = a.beta * (a.scale / (float)a.K);
   TeamSums<2> sums(&s_team, cl);
-  LossTotals t = {};
+  // over the team's pairs, as PolicySums; the team's first thread's
+  __shared__ Sum2 s_pairs[BLOCK ? 1 : kWarpTeams][4];
+  Sum2* const f = s_pairs[BLOCK ? 0 : warp];
+  if (tid == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = {};
+  }
+  uint32_t right = 0;
   const auto span_of = [&](uint32_t k, int i, uint32_t c0) {
     const PrefSide& sd = a.side[i];
     return Span<MODE>(k, c0, threads, tid, sd.T, sd.lp.row, sd.phase);
@@ -798,6 +830,7 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
       for (int i = 0; i < 2; ++i) {
         const PrefSide& sd = a.side[i];
         uint32_t c0 = chunk0;
+        Sum2 row = {};
         do {
           const Span<MODE> c = span_of(k, i, c0);
           bits[i] = load_mask<MODE>(sd.mask, c);
@@ -809,10 +842,13 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
 #pragma unroll
             for (int j = 0; j < kE; ++j) x[j] -= y[j];
           }
+          float part = 0.f;
 #pragma unroll
-          for (int j = 0; j < kE; ++j) s[i] += (bits[i] >> j) & 1u ? x[j] : 0.f;
+          for (int j = 0; j < kE; ++j) part += (bits[i] >> j) & 1u ? x[j] : 0.f;
+          row.add(part);
           c0 += stride;
         } while (c0 < (uint32_t)sd.T + 7);
+        s[i] = row.value();
       }
     }
     sums.template sum<TEAM>(n, s, true);
@@ -822,11 +858,11 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
     const Pair p = pair_of(a, sc, sr);
     if (tid == 0 && rank == 0) {
       if (a.margins) a.margins[k] = p.h;
-      t.f[0] += p.loss;
-      t.f[1] += p.h;
-      t.f[2] += sc;
-      t.f[3] += sr;
-      t.c[0] += p.h > 0.f ? 1 : 0;
+      f[0].add(p.loss);
+      f[1].add(p.h);
+      f[2].add(sc);
+      f[3].add(sr);
+      right += p.h > 0.f ? 1 : 0;
     }
     if (!a.side[0].d.p) continue;
 #pragma unroll
@@ -849,6 +885,8 @@ __global__ void __launch_bounds__(most_threads(TEAM), blocks_per_sm(MODE, TEAM))
     __syncwarp();
     cluster_sync();
   }
+  LossTotals t = {};
+  if (tid == 0) t = {{f[0].value(), f[1].value(), f[2].value(), f[3].value()}, {right, 0, 0}};
   if (!grid_totals(a.w, t)) return;
   const float K = (float)a.K;
   const float loss = a.scale * (t.f[0] / K);
@@ -892,7 +930,7 @@ unsigned loss_blocks(int64_t blocks, int threads, int cluster, int resident, int
 
 template <class Args>
 cudaError_t launch_team(void (*kernel)(Args), unsigned grid, unsigned threads, int cluster,
-                        cudaStream_t s, const Args& a) {
+                        size_t shared, cudaStream_t s, const Args& a) {
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -902,6 +940,7 @@ cudaError_t launch_team(void (*kernel)(Args), unsigned grid, unsigned threads, i
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid, 1, 1);
   cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = shared;
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
@@ -981,7 +1020,8 @@ cudaError_t launch_policy_loss(const PolicyArgs& args, int num_sms, cudaStream_t
   return launch_team(m == kEights    ? policy_kernel<kEights>(t.kind)
                      : m == kShifted ? policy_kernel<kShifted>(t.kind)
                                      : policy_kernel<kSingle>(t.kind),
-                     grid, (unsigned)threads, t.cluster, s, a);
+                     grid, (unsigned)threads, t.cluster, block ? 3 * sizeof(Sum2) * threads : 0, s,
+                     a);
 }
 
 cudaError_t launch_preference_loss(const PrefArgs& args, int num_sms, cudaStream_t s) {
@@ -1004,7 +1044,7 @@ cudaError_t launch_preference_loss(const PrefArgs& args, int num_sms, cudaStream
   return launch_team(m == kEights    ? preference_kernel<kEights>(t.kind)
                      : m == kShifted ? preference_kernel<kShifted>(t.kind)
                                      : preference_kernel<kSingle>(t.kind),
-                     grid, (unsigned)threads, t.cluster, s, a);
+                     grid, (unsigned)threads, t.cluster, 0, s, a);
 }
 
 }  // namespace bgpo
