@@ -16,7 +16,9 @@
  * launches on `stream`, no allocation, host-side checks before any launch, a status
  * for each call, device-detected faults in the error word of the workspace
  * (bgpo_get_device_error, bgpo_clear_device_error). Results are deterministic: sums
- * have a fixed order and no atomic decides one.
+ * have a fixed order and no atomic decides one. The sums of the losses and of the norm
+ * are fp32 in trees of a bounded depth; where a chain grows with the sizes it carries what
+ * its roundings leave out, so that their error does not grow with the batch.
  */
 #ifndef BGPO_TRAIN_H_
 #define BGPO_TRAIN_H_
@@ -64,10 +66,14 @@ bgpo_status bgpo_token_logp_fwd(const bgpo_problem* prob, const uint8_t* mask, c
 /*
  * Gradient of sum dlogp[b, i] logp[b, i] over the tokens that the preceding
  * bgpo_token_logp_fwd on this workspace selected (same prob, X, W and Y):
- *   dz_r = dlogp_r (onehot(y_r) - softmax(W x_r))   (bf16)
+ *   dz_r = dlogp_r (onehot(y_r) - softmax(W x_r))
  *   dX[b, i] = W^T dz_r (0 where not selected),  dW = sum_r dz_r x_r^T
  * Both are sums in fp32 rounded once to bf16, the type of X and W: what a bf16 network's
- * backward takes. They are written whole, not accumulated; dlogp of positions that were
+ * backward takes. dz is rounded to bf16 before the two products, as their tensor cores
+ * take it (like W and X): beyond 128 selected tokens dX and dW are 0.0024 of their norm off,
+ * of which bf16 outputs alone make 0.0017. Up to 128 tokens, where one entry's rounding
+ * would show, what it leaves out goes through the products too, and only the outputs'
+ * rounding is left. They are written whole, not accumulated; dlogp of positions that were
  * not selected is not read. May be repeated with another dlogp.
  *   dlogp device float [B, R];  dX device bf16 [B, R, H], dW device bf16 [V, H], 16-byte
  *   aligned
@@ -110,7 +116,9 @@ bgpo_status bgpo_train_workspace_clear(void* ws, size_t ws_bytes, void* stream);
  * A token is clipped when A > 0 and r > 1 + clip_high, or A < 0 and r < 1 - clip_low.
  * With BGPO_RATIO_SEQUENCE the gradient flows through the row's ratio; since r_b is a
  * mean, each of the row's tokens gets -w_b A_b r_b as above. A row without tokens
- * contributes nothing. Values of masked-out tokens are not read; their dlogp is 0.
+ * contributes nothing. Values of masked-out tokens are never used, and their dlogp is 0; they
+ * may be loaded beside tokens that count, so that all N T elements have to be readable (and
+ * not being written meanwhile).
  *   logp, logp_old, logp_ref, adv   float; logp_ref optional (then beta must be 0);
  *       adv with col = 0 is one advantage a row, which BGPO_RATIO_SEQUENCE requires
  *   mask    uint8, nonzero = the token counts; optional (every token counts)
@@ -148,7 +156,8 @@ bgpo_status bgpo_policy_loss(const bgpo_policy_loss_args* args, void* ws, size_t
  *   L   = scale / K sum_k loss(h_k)
  *   d_chosen = dL/dlogp = m loss'(h) beta scale / K (/ n),  d_rejected = the negative
  *       with the rejected row's m and n
- * A row without tokens has S = 0.
+ * A row without tokens has S = 0. Values of masked-out tokens are never used but may be
+ * loaded, as in bgpo_policy_loss; their gradients are 0.
  *   chosen, rejected           float [K, T_chosen], [K, T_rejected]
  *   ref_*                      float, both or neither (then S = sum m logp)
  *   mask_*                     uint8, nonzero = the token counts; each optional
@@ -199,8 +208,9 @@ typedef struct bgpo_grad {
 /*
  * norm_out = sqrt(sum of the squares of all elements of all gradients): the Euclidean
  * norm, as one device float. Squares and their sums within a unit of 8,192 elements are
- * fp32; sums of those carry what their roundings leave out. Elements beyond 1.8e19 in
- * magnitude overflow to an infinite norm, and elements below 1e-23 count as zero. An empty
+ * fp32; sums of those carry what their roundings leave out. A norm beyond 1.8e19 comes out
+ * infinite; squares below 1e-38 (elements below 1e-19) lose bits, and elements below 2e-23
+ * count as zero. An empty
  * list has norm 0. A non-finite norm sets the device error word to BGPO_ERR_NONFINITE (the
  * value is still written).
  * `out` and `out_type` are not used; trace is optional. n of a tensor at most 2^40, of the

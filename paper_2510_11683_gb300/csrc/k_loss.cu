@@ -7,21 +7,28 @@
 // work of one team: a warp up to 256 tokens, a block of up to 512 threads up to 4,096, a
 // cluster of up to 8 such blocks beyond. Each thread of a team holds 8 tokens in
 // registers while the team's sums go through shuffles, shared memory and the cluster's
-// shared memory, then writes their gradients: every input is read once (rows of more than
-// 32,768 tokens are read again, from L2 where it holds them). Where a loss needs no sum
-// over a row its chunks of 256 tokens are dealt to warps. The mean over all tokens of a
-// masked batch needs their count first, which a kernel of its own takes from the mask.
-// Blocks leave their shares of the loss; the last to finish adds them up in block order.
+// shared memory, then writes their gradients: every input is read once. (A row of more than
+// 32,768 tokens is read twice by one cluster, both times with loads that ask L2 to let go of
+// their lines first: 64 rows of 40,000, half of the tokens counting, 24 us; 4 of 10^6 without
+// a mask 55.) Where a loss needs no sum over a row its chunks of 256 tokens are dealt to
+// warps. The mean over all tokens of a masked batch needs their count first, which a kernel
+// of its own takes from the mask. Blocks leave their shares of the loss; the last to finish
+// adds them up in block order.
 //
 // The mask comes first: values of tokens that do not count are never used, and not loaded
 // but beside ones that do. Arrays that run along memory move in vectors of eight tokens.
 //
+// Sums are fp32 in trees of a bounded depth (a thread's eight, a warp, a block, a cluster, the
+// blocks); chains whose length grows with the batch or the row carry what their roundings
+// leave out.
+//
 // What bounds them: HBM where a batch outgrows L2 (policy loss with KL, 4096 x 4096 tokens
-// without a mask: 44 us for 268 MB, 6.2 TB/s; with ragged rows and the mean by rows, 59% of
-// the tokens counting: 40 us for 202 MB, a team's barrier and the longest row of a round
+// without a mask: 44 us for 268 MB, 6.1 TB/s; with ragged rows and the mean by rows, 59% of
+// the tokens counting: 43 us for 202 MB, a team's barrier and the longest row of a round
 // beside it), the chain mask - values - sums - gradient and a few rounds of teams below
-// (preference loss, 1024 pairs of 2,047: 16 us for 40 MB), and the host's 8 to 12 us a call
-// for all smaller ones.
+// (preference loss, 1024 pairs of 2,047: 16 us for 40 MB; policy loss, 512 x 1023 with the mean
+// over tokens: 8.6 for both kernels, from L2), and for smaller ones the host: 8 to 12 us in the
+// call, and as much again in a caller's transposed views of Monte Carlo samples.
 #include <math.h>
 
 #include "bgpo_device.cuh"
@@ -43,7 +50,7 @@ __device__ __forceinline__ int32_t warp_sum_i(int32_t v) {
   return (int32_t)__reduce_add_sync(0xffffffffu, (unsigned)v);
 }
 
-// (read once: 44.4 -> 42.0 us at 4096 x 4096 with ragged rows)
+// (for what is read once; when it came, 44.4 -> 42.0 us at 4096 x 4096 with ragged rows)
 __device__ __forceinline__ void load8(const float* p, float (&v)[kE]) {
   asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.f32 "
                "{%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -199,7 +206,9 @@ enum TeamKind : int { kNone = 0, kWarp = 1, kBlock = 2, kCluster = 3, kMany = 4 
 // may take: 85 a thread for warps on their own (24 an SM; at 64, spills made 4096 x 4096
 // tokens without a mask take 52 us instead of 43), 64 in blocks (one block of 512 threads
 // and 128 registers instead of two: 45 us instead of 41 at 4096 x 4096 ragged), 128 for
-// single tokens, whose addresses take more.
+// single tokens, whose addresses take more. What still spills, in bytes a thread: policy
+// kernels of blocks and clusters 28 to 44, of single tokens 36; preference kernels of blocks
+// up to 12, of single tokens 268.
 constexpr int most_threads(int team) { return team >= kBlock ? kMaxThreads : 32 * kWarpTeams; }
 constexpr int blocks_per_sm(int mode, int team) {
   return team >= kBlock ? (mode == kSingle ? 1 : 2) : (mode == kSingle ? 2 : 3);
@@ -357,7 +366,7 @@ __global__ void __launch_bounds__(32 * kWarpTeams)
 
 // e^k - 1 - k for |k| <= 1. It is k^2 / 2 for small k, where the difference would keep few
 // of its bits (none below k = 2e-4): the series of e^k, whose first left-out term is below
-// 2^-24 of it.
+// 1.2 x 2^-24 of it (most at k = -1).
 __device__ __forceinline__ float exp_rest(float k) {
   float p = fmaf(k, 1.f / 3628800.f, 1.f / 362880.f);
   p = fmaf(k, p, 1.f / 40320.f);
@@ -442,8 +451,8 @@ struct Side {
         bound(A > 0.f ? a.hi : A < 0.f ? -a.lo : INFINITY) {}
 };
 
-// Instructions come next after HBM (120 a token took 94 us at 4096 x 4096, 67 took 48, 40 take
-// 39): what is the same for all tokens is asked once a unit, a warp whose tokens all count
+// Instructions come next after HBM (120 a token took 94 us at 4096 x 4096, 67 took 48, 40 took
+// 39; the sums' remainders and the mask in them made it 45 and 41): what is the same for all tokens is asked once a unit, a warp whose tokens all count
 // tests none of them, and two values go through one instruction where they can. A token that
 // does not count has log ratios 0: its ratio is 1, inside every clipping range, and is dropped
 // before the sums (adding it and taking a count of them out again would leave an absolute
@@ -920,7 +929,7 @@ int resident(Mode m, TeamKind t) { return blocks_per_sm(m, t) * most_threads(t);
 
 // Blocks of a launch: as many as there is work for, at most what the device holds at once
 // with `resident` threads an SM: later units then find their masks loaded. (Twice as many
-// blocks: 17 us instead of 14 at 1024 pairs x 2,047.)
+// blocks, when tried: 17 us instead of 14 at 1024 pairs x 2,047.)
 unsigned loss_blocks(int64_t blocks, int threads, int cluster, int resident, int num_sms) {
   int64_t most = (int64_t)num_sms * (resident / threads);
   if (most > kTrainMaxBlocks) most = kTrainMaxBlocks;

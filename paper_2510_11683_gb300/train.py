@@ -38,7 +38,7 @@ def token_logp_fwd(prob, X, W, Y, ws, logp, mask=None, stream=None):
 def token_logp_bwd(prob, W, dlogp, ws, dX, dW, stream=None):
     """dX (bfloat16 [B, R, H]) and dW (bfloat16 [V, H]) = gradients of sum dlogp logp over the
     tokens that the preceding token_logp_fwd on ws selected; dX is 0 elsewhere. Both are
-    written whole."""
+    written whole. Beyond 128 tokens dL/dz is rounded to bf16 between the products."""
     torch, cur = _torch(), _current_device()
     n = prob.B * prob.R
     st = _lib.lib().bgpo_token_logp_bwd(
@@ -123,7 +123,8 @@ def policy_loss(logp, logp_old, A, out, dlogp, ws, logp_ref=None, mask=None, cli
 
     logp, logp_old, logp_ref (optional), dlogp (None: the loss alone): float32 [N, T];
     A: float32 [N] or [N, T]; mask: bool or uint8 [N, T], True where a token counts; out:
-    float32 [6] = loss, policy term, KL term, share clipped below and above, mean ratio.
+    float32 [6] = loss, policy term, KL term, share clipped below and above, mean ratio. What
+    stands at masked-out tokens is never used (but has to be readable); their dlogp is 0.
     ratio: "token", or "sequence" (one ratio a row, from its mean log ratio). norm: "rows"
     (mean over rows of their tokens' mean), "tokens" (mean over tokens), "sum"."""
     shape = _pair_shape(logp, "logp")
@@ -239,8 +240,8 @@ def _grad_type(t, name):
 
 def grad_set(grads, into=None):
     """GradSet over contiguous CUDA tensors (float32, bfloat16, float16; of any sizes, zero
-    included). into: a tensor of the same size for each clipped gradient, of any of the
-    types (None: the gradients are clipped in place)."""
+    included), each listed once. into: a tensor of the same size for each clipped gradient, of
+    any of the types (None: the gradients are clipped in place)."""
     torch, cur = _torch(), _current_device()
     grads = list(grads)
     into = grads if into is None else list(into)
